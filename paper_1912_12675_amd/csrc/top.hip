@@ -423,7 +423,18 @@ struct Cut {
             splits = (int)((bytes + 16 * per - 1) / (16 * per));
         }
     }
+    // of the workspace: the pieces' first k and sums
+    size_t ws_bytes(int n, int k) const { return splits > 1 ? (size_t)n * splits * (k * sizeof(u64) + sizeof(float2)) : 0; }
 };
+
+// Calls f(cut) for each way in which rows of these sizes can be cut: either type, with and without a chunk more for rows
+// that begin inside one.  More bytes can mean fewer pieces (33 small ones of 128 entries turn to 17 large ones).
+template <typename F>
+void each_cut(int n, int classes, int k, F f)
+{
+    for (int size : {2, 4})
+        for (int64_t bytes : {(int64_t)classes * size, row_bytes(classes, size)}) f(Cut(n, bytes, k));
+}
 
 template <typename E>
 void launch(const TopArgs& a, int64_t bytes, const Work& w, hipStream_t st)
@@ -469,16 +480,15 @@ void launch(const TopArgs& a, int64_t bytes, const Work& w, hipStream_t st)
 size_t top_logits_ws_bytes(int n, int classes, int k)
 {
     size_t need = 0;
-    for (int size : {2, 4}) {
-        const Cut c(n, row_bytes(classes, size), k);
-        if (c.splits > 1) need = std::max(need, (size_t)n * c.splits * ((size_t)k * sizeof(u64) + sizeof(float2)));
-    }
+    each_cut(n, classes, k, [&](const Cut& c) { need = std::max(need, c.ws_bytes(n, k)); });
     return need;
 }
 
 bool top_logits_fits(int n, int classes, int k)
 {
-    return (int64_t)n * std::max(Cut(n, row_bytes(classes, 2), k).splits, Cut(n, row_bytes(classes, 4), k).splits) <= INT32_MAX;
+    int64_t most = 0;
+    each_cut(n, classes, k, [&](const Cut& c) { most = std::max(most, (int64_t)n * c.splits); });
+    return most <= INT32_MAX;
 }
 
 hipError_t top_logits(int n, int classes, int bf16, const void* z, int64_t ld, int k, float tau, float* val, int32_t* idx,
