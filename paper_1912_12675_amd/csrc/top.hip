@@ -359,7 +359,9 @@ __global__ __launch_bounds__(T) void top_merge_k(TopArgs a)
         m = block_reduce<T>(m, sh[0], [](float x, float y) { return fmaxf(x, y); });
         for (int i = tid; i < a.splits; i += T) {
             const float2 f = part[i];
-            s += f.x == m ? f.y : f.y * __builtin_amdgcn_exp2f((base(f.x) - base(m)) * kt);
+            // a piece without a logit above -inf adds nothing (or a NaN): relative to a row far below 0 its base, 0, is infinite
+            const bool as_is = f.x == m || f.x == -INFINITY;
+            s += as_is ? f.y : f.y * __builtin_amdgcn_exp2f((base(f.x) - base(m)) * kt);
         }
         s = block_reduce<T>(s, sh[1], [](float x, float y) { return x + y; });
         if (tid == 0) a.lse[row] = (float)((double)base(m) * a.inv_tau + log_of((double)s));

@@ -1,10 +1,10 @@
 """Top logits and the distillation loss where their rules change: workspaces of exactly the bytes that are asked for, masked
-pieces of rows far from zero, a loss of labels alone."""
+pieces of rows far from zero."""
 import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_distill import matrix, top_ref
+from tests.test_gpu_distill import check_top, matrix, top_ref
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +37,32 @@ def test_top_logits_workspace(P, n, c, k, type_, pad):
     np.testing.assert_array_equal(val.double().cpu().numpy(), v)
     # as in check_top: 300 half steps of the terms' sum, and one rounding
     assert (np.abs(lse.double().cpu().numpy() - want) <= 300 * 2.0**-24 + 2.0**-24 * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("type_", ["f32", "bf16"])
+@pytest.mark.parametrize("n,c,k,pad,tau,at,spread,masked", [
+    (2, 70000, 5, 0, 0.046875, -8.6, 0.0, 464),      # a short last piece that a mask covers
+    (3, 262144, 40, 0, 1.0, -1000.0, 3.0, 100000),
+    (130, 140000, 3, 1, 2.0**-7, -5.0, 1.0, 70000),
+    (2, 131072, 128, 1, 1.0, -300.0, 3.0, 0),    # rows that begin inside 16 bytes have a piece more, the others' is empty
+    (1, 1 << 20, 256, 0, 2.0**-16, -1.0, 0.5, 1 << 19)])
+def test_masked_pieces_far_from_zero(P, n, c, k, pad, tau, at, spread, masked, type_):
+    """Pieces of a row that hold nothing, and a largest logit below -89 T: the exponential of its distance from 0 has no
+    number, and is not to be multiplied by the empty piece's sum."""
+    print(f"masked pieces {n}x{c} k {k} {type_} pad {pad} T {tau} at {at}", flush=True)
+    rng = np.random.default_rng(c)
+    z = at + rng.standard_normal((n, c)) * spread
+    z[:, c - masked:] = -np.inf
+    x, _ = matrix(z, type_, pad)
+    check_top(P, x, k, tau, "masked pieces")
+    x[n - 1] = -float("inf")
+    check_top(P, x, k, tau, "a row of nothing")
+    if k <= 40:  # the loss takes the sum's logarithm: the teacher is the student, so the loss is 0 up to its rounding
+        z = x[: n - 1].contiguous()
+        val, idx, lse = (torch.zeros(n - 1, k, device="cuda"), torch.zeros(n - 1, k, dtype=torch.int32, device="cuda"),
+                         torch.zeros(n - 1, device="cuda"))
+        P.psw_top_logits(z, val, idx, temperature=tau, lse=lse)
+        row = torch.zeros(n - 1, device="cuda")
+        P.psw_distill(z, idx, val, row_loss=row, t_lse=lse, temperature=tau)
+        torch.cuda.synchronize()
+        assert bool(torch.isfinite(row).all())
