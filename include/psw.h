@@ -236,7 +236,8 @@ size_t psw_q8_quant_ws_bytes(int rows, int cols);
  * Either pair may be NULL.  tiles != 0: square blocks (weights), else blocks of
  * one row each.  A block whose largest finite magnitude is a has the scale 2^E,
  * E the smallest integer >= -126 with a <= 448 * 2^E; a value is x * 2^-E
- * rounded to the nearest e4m3 (ties to even); infinities and NaN become NaN.
+ * rounded to the nearest e4m3 (ties to even), at E = 120 to at most 240, so
+ * that finite numbers stay below 2^128; infinities and NaN become NaN.
  * colsum [cols] (NULL: none) receives sum_r x[r][c] of x itself, not of its
  * rounded values: the bias gradient when x is an output gradient.  ws is read
  * by none of the other outputs and may be NULL without colsum. */

@@ -4,10 +4,11 @@
 // For a block with the largest finite magnitude a, the scale is 2^E with E the
 // smallest integer (at least -126) that has a <= 448 * 2^E, 448 being the
 // largest e4m3; x * 2^-E is then exact and rounds once, to nearest even, by the
-// conversion instruction.  A scale that is a power of two costs no accuracy
-// against a / 448 (a floating-point format's steps are relative) and is what the
-// matrix instruction takes as an operand's scale.  1.75 * 2^8 = 448, so E comes
-// from a's bits: its exponent - 8, and one more where its fraction is past 1.75.
+// conversion instruction (but for numbers nearest to 2^128: below_2_128).  A
+// scale that is a power of two costs no accuracy against a / 448 (a floating-point
+// format's steps are relative) and is what the matrix instruction takes as an
+// operand's scale.  1.75 * 2^8 = 448, so E comes from a's bits: its exponent - 8,
+// and one more where its fraction is past 1.75.
 //
 // A product's depth runs along the rows of one operand and, in the next product,
 // along the columns of the same matrix (dy in dx = dy w and dw = dy^T x), so a
@@ -57,6 +58,16 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d, fl
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * by, d * by, w, true);
 }
 
+// Numbers from 248 * 2^120 on (the lowest of either type, as masks have it) have the largest scale, 2^120, and are nearest to
+// 256 * 2^120 = 2^128, which neither float32 nor bfloat16 has: an infinity in a product, and NaN times a weight of 0.  They
+// become 240 * 2^120, the number below: four rounded values of a block with that scale.
+constexpr uint32_t kLargest = 247;  // its byte
+__device__ __forceinline__ uint32_t below_2_128(uint32_t w)
+{
+    const uint32_t off = (w & 0x7f7f7f7fu) ^ 0x78787878u;    // 0 in bytes of 256
+    return w - ((~(off + 0x7f7f7f7fu) & 0x80808080u) >> 7);  // one less there: no byte borrows
+}
+
 __device__ __forceinline__ float inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
 
 // Four neighbours in one load, which gfx950 takes at any element's address
@@ -76,7 +87,7 @@ __device__ __forceinline__ float4 load4(const T* p)
 // Both orders, column sums, or square blocks: a 128 x 128 tile.  A thread holds
 // two pieces of 4 rows x 4 columns (32 threads side by side read 128 columns of
 // a row): 512 threads a tile leave two to four tiles a CU, of which one loads
-// while others turn (bfloat16 three rather than two: 8192 x 4096 35.5 us, so 34;
+// while others turn (bfloat16 three rather than two: 8192 x 4096 35.5 us, so 34, and 36 with the largest scale's question;
 // float32, whose tiles are twice the bytes, 41 us, with three 47).  Bound by
 // memory: 16384 x 4096 float32, square blocks, 80 us (5.0 TB/s), 8192 x 4096 by
 // rows and columns with sums 41 us (4.9 TB/s); 2047 x 4104 so 17 us (2.9 TB/s;
@@ -176,6 +187,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 6 : 4) void q8_quant_k(Q
         ce[0] = scale_byte(t.x); ce[1] = scale_byte(t.y); ce[2] = scale_byte(t.z); ce[3] = scale_byte(t.w);
     }
 
+    // some block of the tile, whose columns are all in every wave, has the largest scale
+    const bool far = __any(max(max(ce[0], ce[1]), max(ce[2], ce[3])) == kLargest);
     if (a.q) {
         uint8_t* q = a.q + (int64_t)r0 * a.kp + c0;
 #pragma unroll
@@ -226,6 +239,23 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 6 : 4) void q8_quant_k(Q
         else
             a.total[cb * kTile + tid] = (float)s;
     }
+    // Every thread's own words again, from memory: a look at each word's scale as it is made took 5% to 10% of the time, the
+    // numbers changed before registers that bfloat16 has not (8192 x 4096 35 us, so 58).
+    if (far) {
+#pragma unroll 1
+        for (int i = 0; a.q && i < R; ++i) {
+            const int r = 4 * rg + i / 4 * S + i % 4;
+            uint32_t* p = reinterpret_cast<uint32_t*>(a.q + (int64_t)(rb * kTile + r) * a.kp + c0);
+            if (rb * kTile + r < a.rows && (TILES || scale_byte(rowmax[r]) == kLargest)) *p = below_2_128(*p);
+        }
+#pragma unroll 1
+        for (int c = rg; a.qt && c < kTile; c += kThreads / 32) {
+            uint32_t top = 0;
+            for (int w = 0; w < W; ++w) top = max(top, colpart[w][c]);
+            uint32_t* p = reinterpret_cast<uint32_t*>(a.qt + (int64_t)(cb * kTile + c) * a.rp + rb * kTile + 4 * l);
+            if (cb * kTile + c < a.cols && (TILES || scale_byte(top) == kLargest)) *p = below_2_128(*p);
+        }
+    }
 }
 
 // Rows alone (a forward pass): sixteen lanes a block of 128, eight values each,
@@ -272,9 +302,11 @@ __global__ __launch_bounds__(256) void q8_rows_k(QuantArgs a)
         if (row[k] >= a.rows) continue;
         const uint32_t e = scale_byte(m);
         const float by = inverse(e);
-        if (cb[k] < a.cblocks)
-            *reinterpret_cast<uint2*>(a.q + row[k] * a.kp + cb[k] * kTile + 8 * l) =
-                make_uint2(pack4(v[k][0], v[k][1], v[k][2], v[k][3], by), pack4(v[k][4], v[k][5], v[k][6], v[k][7], by));
+        if (cb[k] < a.cblocks) {
+            uint2 w = make_uint2(pack4(v[k][0], v[k][1], v[k][2], v[k][3], by), pack4(v[k][4], v[k][5], v[k][6], v[k][7], by));
+            if (e == kLargest) w = make_uint2(below_2_128(w.x), below_2_128(w.y));
+            *reinterpret_cast<uint2*>(a.q + row[k] * a.kp + cb[k] * kTile + 8 * l) = w;
+        }
         if (l == 0) a.s[row[k] * a.sp + cb[k]] = (uint8_t)(cb[k] < a.cblocks ? e : 127u);
     }
 }

@@ -1,0 +1,85 @@
+"""8-bit operands and products at the ends of their range."""
+import numpy as np
+import pytest
+import torch
+
+from tests import q8_ref
+from tests.test_gpu_q8 import TYPES
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def P():
+    from paper_1912_12675_amd import psw
+    psw.lib()
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    return psw
+
+
+LOWEST = {"f32": -3.4028234663852886e38, "bf16": -3.3895313892515355e38}
+
+
+def stands_for(pair, tiles):
+    """The numbers of an operand's bytes, in 64 bits."""
+    q, s = (t.cpu().numpy() for t in pair)
+    wide = np.repeat(s[:, : q.shape[1] // 128].astype(int) - 127, 128, axis=1)
+    if tiles:
+        wide = np.repeat(wide, 128, axis=0)[: len(q)]
+    return np.ldexp(q8_ref.decode(q), wide)
+
+
+@pytest.mark.parametrize("tiles", [False, True], ids=["rows", "tiles"])
+@pytest.mark.parametrize("type_", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 3), (5, 300), (130, 257)])
+def test_largest_numbers(P, rows, cols, type_, tiles):
+    """Finite numbers become finite ones, below 2^128, in every order and kernel."""
+    print(f"largest numbers {rows}x{cols} {type_} tiles={tiles}", flush=True)
+    rng = np.random.default_rng(rows)
+    x = np.ldexp(rng.uniform(-1, 1, (rows, cols)), rng.integers(100, 129, (rows, cols)))
+    x = np.clip(x, LOWEST[type_], -LOWEST[type_])
+    x[0, 0] = LOWEST[type_]
+    x[rows - 1, cols - 1] = -LOWEST[type_]
+    x[rows // 2, cols // 3] = np.ldexp(247.0 if type_ == "bf16" else 247.99, 120)  # the largest that rounds to 240 * 2^120
+    xt = torch.from_numpy(x.astype(np.float32)).cuda().to(TYPES[type_])
+    x = xt.double().cpu().numpy()
+    q, s = P.q8_operand(rows, cols, tiles)
+    qt, st = P.q8_operand(cols, rows, tiles)
+    P.psw_q8_quant(xt, q, s, qt, st, tiles=tiles)
+    alone = P.q8_operand(rows, cols, tiles)
+    P.psw_q8_quant(xt, *alone, tiles=tiles)
+    torch.cuda.synchronize()
+    assert torch.equal(q, alone[0]) and torch.equal(s, alone[1])
+    for pair, m in (((q, s), x), ((qt, st), x.T)):
+        ref_q, ref_e, _ = q8_ref.quantise(m, tiles)
+        wide = np.repeat(np.repeat(ref_e, 128, axis=1), 128 if tiles else 1, axis=0)[: len(m)]
+        ref = np.ldexp(ref_q, wide)
+        assert (np.abs(ref) >= 2.0**128).any()  # the nearest: past every float
+        ref = np.clip(ref, -240 * 2.0**120, 240 * 2.0**120)
+        np.testing.assert_array_equal(stands_for(pair, tiles), ref)
+
+
+@pytest.mark.parametrize("type_", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [5, 20, 100])
+def test_masked_inputs(P, n, type_):
+    """Inputs of the type's lowest number under weights of 0 add nothing; under a tiny weight an ordinary number."""
+    print(f"masked inputs {n} {type_}", flush=True)
+    rng = np.random.default_rng(n)
+    fin, out = 300, 70
+    x = rng.standard_normal((n, fin))
+    x[:, 128:200] = LOWEST[type_]
+    w = rng.standard_normal((out, fin))
+    w[:, 128:256] = 0.0
+    w[:, 130] = 2.0**-120
+    x8, w8 = P.q8_operand(n, fin), P.q8_operand(out, fin, True)
+    P.psw_q8_quant(torch.from_numpy(x.astype(np.float32)).cuda().to(TYPES[type_]), *x8)
+    P.psw_q8_quant(torch.from_numpy(w.astype(np.float32)).cuda(), *w8, tiles=True)
+    y = torch.zeros(n, out, dtype=TYPES[type_], device="cuda")
+    P.psw_fc8_fwd(x8, w8, fin, y)
+    torch.cuda.synchronize()
+    a, b = stands_for(x8, False), stands_for(w8, True)
+    want, size, square = a @ b.T, np.abs(a) @ np.abs(b).T, np.sqrt((a * a) @ (b * b).T)
+    # fp32: a step of 2^-23 for each addition; bfloat16: half a step, and seven times the 7e-5 of the root of the
+    # products' squares that the 8-bit instruction was measured to drop
+    bound = (fin + 8) * 2.0**-23 * size if type_ == "f32" else 2.0**-8 * np.abs(want) + (1 + 2.0**-8) * 2.0**-11 * square
+    assert (np.abs(y.double().cpu().numpy() - want) <= bound).all()
