@@ -221,8 +221,9 @@ enum { PSW_T_F32 = 0, PSW_T_BF16 = 1 };
  *     PSW_Q8_BLOCK of the depth (of one row, or of as many rows); sp = kp /
  *     PSW_Q8_BLOCK rounded up to 4, bytes of 127 behind the last block; 4-byte
  *     aligned.
- * Its elements are value * scale.  psw_q8_sizes gives the bytes of both arrays
- * (host outputs). */
+ * Its elements are value * scale, below 2^128 in magnitude (or NaN), as
+ * psw_q8_quant makes them.  psw_q8_sizes gives the bytes of both arrays (host
+ * outputs). */
 #define PSW_Q8_BLOCK 128
 int psw_q8_sizes(int rows, int k, int tiles, int64_t *value_bytes, int64_t *scale_bytes);
 
@@ -250,18 +251,23 @@ size_t psw_fc8_ws_bytes(int n, int in, int out);
 
 /* psw_fc_fwd of 8-bit operands: y[n,o] = b[o] + sum_i x[n,i] w[o,i], then
  * max(0,.) if relu; y [n][out] of `type`.  x: n rows of depth in; w: out rows
- * of depth in, square blocks.  A float32 y is the exact products' sum in fp32;
- * a bfloat16 y comes of the 8-bit matrix instruction, which drops low bits of
- * small products beside large ones (about 2^-14 of a result, against the 2^-9 of
- * the rounding that follows).  The sums are formed in a fixed order: results
- * are bit-reproducible. */
+ * of depth in, square blocks.  A float32 y is the sum of exact products in fp32;
+ * elements below 2^-133 (of scales 2^-126 and 2^-125) count as the nearest
+ * multiple of 2^-133.  A bfloat16 y comes of the 8-bit matrix instruction, which
+ * drops low bits of small products beside large ones: about 2^-14 of the root of
+ * the sum of the products' squares.  Beside the rounding that follows, up to
+ * 2^-8 of the result, that is little where the result is as large as that root,
+ * and the larger part where the products cancel to a sixtieth of it.  Few rows (up
+ * to 16, and up to 64 where that is faster) are exact sums for either type.  The
+ * sums are formed in a fixed order, which goes by the sizes and the type alone:
+ * results are bit-reproducible. */
 int psw_fc8_fwd(int n, int in, int out, const uint8_t *xq, const uint8_t *xs, const uint8_t *wq,
                 const uint8_t *wsc, const float *b, int relu, int type, void *y, void *ws,
                 size_t ws_bytes, void *stream);
 
 /* dx[n,i] (+)= sum_o dy[n,o] w[o,i]: dy n rows of depth out; wt the transposed
- * weights, in rows of depth out, square blocks; dx [n][in] of `type`,
- * overwritten (accumulate == 0) or added to. */
+ * weights, in rows of depth out, square blocks; dx [n][in] of `type` (by it the
+ * sums are as psw_fc8_fwd's), overwritten (accumulate == 0) or added to. */
 int psw_fc8_bwd_data(int n, int in, int out, const uint8_t *dyq, const uint8_t *dys, const uint8_t *wtq,
                      const uint8_t *wts, int type, void *dx, int accumulate, void *ws, size_t ws_bytes,
                      void *stream);

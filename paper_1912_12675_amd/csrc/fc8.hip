@@ -6,13 +6,15 @@
 //  - bfloat16 results: v_mfma_scale_f32_32x32x64_f8f6f4, which takes e4m3 values
 //    and the scales' exponents as they are, 4.7 PFLOP/s on this card.  It aligns
 //    the products of a few neighbouring k to the largest of them and drops what
-//    falls below: measured on normal, half-normal and long-tailed operands a
-//    result of 1.5e-5 to 7e-5 relative error (any depth, any of the 8-bit
-//    instructions), a fiftieth of bfloat16's own rounding, 2^-9 to 2^-8.
-//  - float32 results: the values times their scales as bfloat16 (e4m3 has four
-//    significant bits, so that is exact) by v_cvt_scalef32_pk_bf16_fp8, and
-//    v_mfma_f32_32x32x16_bf16, whose products are exact and whose sums are
-//    fp32: 1e-8 to 4e-7 on the same operands, at 2.45 PFLOP/s.
+//    falls below: measured on normal, half-normal and long-tailed operands an
+//    error of 1.5e-5 to 7e-5 of the root of the summed squares (any depth, any of
+//    the 8-bit instructions), a fiftieth of bfloat16's own rounding, 2^-9 to 2^-8 of
+//    a result that is as large.
+//  - float32 results, and few rows of either type: the values times their scales
+//    as bfloat16 (e4m3 has four significant bits, so that is exact from 2^-133,
+//    bfloat16's smallest, up to below 2^128) by v_cvt_scalef32_pk_bf16_fp8, and
+//    v_mfma_f32_32x32x16_bf16, whose products are exact, of subnormal numbers too,
+//    and whose sums are fp32: 1e-8 to 4e-7 on the same operands, at 2.45 PFLOP/s.
 #include <algorithm>
 #include <type_traits>
 

@@ -1,4 +1,4 @@
-"""8-bit operands and products at the ends of their range."""
+"""8-bit operands and products at the ends of their range, and what the 8-bit instruction drops."""
 import numpy as np
 import pytest
 import torch
@@ -83,3 +83,56 @@ def test_masked_inputs(P, n, type_):
     # products' squares that the 8-bit instruction was measured to drop
     bound = (fin + 8) * 2.0**-23 * size if type_ == "f32" else 2.0**-8 * np.abs(want) + (1 + 2.0**-8) * 2.0**-11 * square
     assert (np.abs(y.double().cpu().numpy() - want) <= bound).all()
+
+
+@pytest.mark.parametrize("n", [16, 32, 256])
+def test_exact_range(P, n):
+    """One product a result, so that a float32 result is exact wherever the operand's element is a bfloat16 number: every
+    e4m3 value at scales over their whole range, with value * scale from 2^-133 up to below 2^128.  Below, an element is off
+    by at most half of 2^-133."""
+    fin, out = 1024, 64
+    for lo in (1, 9, 64, 124, 190, 240, 247):
+        print(f"exact range {n} rows, scales from {lo}", flush=True)
+        e = np.minimum(lo + np.arange(8), 254)
+        down = -100 if lo >= 127 else 100
+        w8 = torch.full((out, fin), 0x38, dtype=torch.uint8, device="cuda"), torch.full((1, 8), 127 + down, dtype=torch.uint8, device="cuda")
+        s = torch.from_numpy(np.tile(e.astype(np.uint8), (n, 1))).cuda()
+        for start in range(0, 256, n):
+            for turn in range(8):
+                m = np.arange(n)
+                at = (m + turn) % 8
+                v = ((start + m) % 256).astype(np.uint8)
+                v[(v & 127) == 127] = 0
+                for _ in range(16):  # an exponent less until the element is below 2^128
+                    v = np.where(np.ldexp(np.abs(q8_ref.decode(v)), e[at] - 127) >= 2.0**128, v - 8, v).astype(np.uint8)
+                q = np.zeros((n, fin), np.uint8)
+                q[m, at * 128 + (37 * m + turn) % 128] = v
+                y = torch.zeros(n, out, device="cuda")
+                P.psw_fc8_fwd((torch.from_numpy(q).cuda(), s), w8, fin, y)
+                torch.cuda.synchronize()
+                element = np.ldexp(q8_ref.decode(v), e[at] - 127)
+                off = np.abs(y.double().cpu().numpy() - np.ldexp(element, down)[:, None])
+                whole = np.ldexp(element, 133) == np.round(np.ldexp(element, 133))  # numbers that bfloat16 has
+                assert (off[whole] == 0).all(), (lo, element[whole][(off[whole] > 0).any(1)])
+                assert (off <= 2.0**(down - 134)).all(), (lo, off.max())
+
+
+@pytest.mark.parametrize("n,fin,out", [(20, 2000, 300), (64, 4096, 512), (128, 4096, 640), (700, 1024, 520), (2100, 512, 2050)])
+def test_bfloat16_products_in_the_norm(P, n, fin, out):
+    """Against the nearest bfloat16 numbers of the exact results.  The 8-bit instruction drops at most d = 7e-5 of the root
+    of the summed squares (measured); a result so becomes the neighbouring number, a step of at most 2^-7 away, with
+    probability d / step, which leaves a mean square of d step, and d^2 where the result is smaller than d.  Twice that
+    for chance."""
+    print(f"norm {n}x{fin}->{out}", flush=True)
+    rng = np.random.default_rng(n)
+    x8, w8 = P.q8_operand(n, fin), P.q8_operand(out, fin, True)
+    P.psw_q8_quant(torch.from_numpy(rng.standard_normal((n, fin)).astype(np.float32)).cuda(), *x8)
+    P.psw_q8_quant(torch.from_numpy(rng.standard_normal((out, fin)).astype(np.float32)).cuda(), *w8, tiles=True)
+    y = torch.zeros(n, out, dtype=torch.bfloat16, device="cuda")
+    P.psw_fc8_fwd(x8, w8, fin, y)
+    torch.cuda.synchronize()
+    a, b = torch.from_numpy(stands_for(x8, False)).cuda(), torch.from_numpy(stands_for(w8, True)).cuda()
+    want, square = a @ b.t(), (a.square() @ b.square().t()).sqrt()
+    d = 7e-5 * square
+    off = (y.double() - want.to(torch.bfloat16).double()).square().sum()
+    assert float(off) <= 2 * float((d * 2.0**-7 * want.abs() + d.square()).sum())
