@@ -208,7 +208,10 @@ int psw_dropout(int64_t count, const float *in, float *out, int accumulate, int 
 /* Fully connected products in 8 bits, with a scale for each block of 128.  */
 /* ------------------------------------------------------------------------ */
 
-/* Storage types of the entry points below that take matrices as void*. */
+/* Storage types of the entry points below that take matrices as void*.  What
+ * would take 2^32 threads of one launch is refused with PSW_ERR_SHAPE: 2^27 rows
+ * of up to 512 columns to quantise, 2^27 columns of a product of up to 16 rows,
+ * 2^26 rows of up to 1000 float32 logits, or 2^23 of 10000. */
 enum { PSW_T_F32 = 0, PSW_T_BF16 = 1 };
 
 /* An 8-bit operand of `rows` rows of depth k (the summed index of a product)

@@ -462,8 +462,7 @@ int psw_q8_quant(int rows, int cols, int type, const void* x, int64_t ld, int ti
     if (!e) e = check_type("q8_quant", type);
     if (e) return e;
     if (ld < cols) return fail(PSW_ERR_SHAPE, "q8_quant: ld < cols");
-    if (psw::q8_depth(rows) / psw::kQ8Block * (psw::q8_depth(cols) / psw::kQ8Block) > INT32_MAX ||
-        (int64_t)rows * psw::q8_scales(cols) / 32 >= INT32_MAX)
+    if (!psw::q8_quant_fits(rows, cols, !tiles && !qt && !colsum))
         return fail(PSW_ERR_SHAPE, "q8_quant: matrix too large");
     if (!x || (!q != !s) || (!qt != !st) || (!q && !qt && !colsum))
         return fail(PSW_ERR_NULL, "q8_quant: x, and q with s, qt with st, or colsum, are required");
@@ -490,11 +489,12 @@ static int check_mm8(const char* what, int M, int N, int depth, int type, const 
     if (!e) e = check_type(what, type);
     if (e) return e;
     if (depth > 1 << 23) return fail(PSW_ERR_UNSUPPORTED, "%s: summed size above 2^23", what);
+    if (((int64_t)M + 15) / 16 * (((int64_t)N + 15) / 16) > INT32_MAX || !psw::mm8_fits(M, N, depth, type == PSW_T_BF16))
+        return fail(PSW_ERR_SHAPE, "%s: result too large", what);
     if (!a || !sa || !b || !sb || !c) return fail(PSW_ERR_NULL, "%s: operands and result are required", what);
     if ((uintptr_t)a % 16 || (uintptr_t)b % 16 || (uintptr_t)sa % 4 || (uintptr_t)sb % 4 ||
         (uintptr_t)c % (type == PSW_T_BF16 ? 2 : 4))
         return fail(PSW_ERR_SHAPE, "%s: values must be aligned to 16 bytes, scales to 4, the result to its elements", what);
-    if (((int64_t)M + 15) / 16 * (((int64_t)N + 15) / 16) > INT32_MAX) return fail(PSW_ERR_SHAPE, "%s: result too large", what);
     const size_t need = psw::mm8_ws_bytes(M, N, depth);
     if (need && (!ws || (uintptr_t)ws % 16)) return fail(PSW_ERR_NULL, "%s: needs a workspace aligned to 16 bytes", what);
     if (ws_bytes < need) return fail(PSW_ERR_WORKSPACE, "%s: workspace %zu < %zu bytes", what, ws_bytes, need);
@@ -557,8 +557,8 @@ int psw_top_logits(int n, int classes, int type, const void* logits, int64_t ld,
     const int e = check_logits("top_logits", n, classes, type, logits, ld, k, temperature);
     if (e) return e;
     if (k > classes) return fail(PSW_ERR_SHAPE, "top_logits: k > classes");
+    if (!psw::top_logits_fits(n, classes, k, type == PSW_T_BF16)) return fail(PSW_ERR_SHAPE, "top_logits: too many rows");
     if (!val || !idx) return fail(PSW_ERR_NULL, "top_logits: val and idx are required");
-    if (!psw::top_logits_fits(n, classes, k)) return fail(PSW_ERR_SHAPE, "top_logits: too many rows");
     const size_t need = psw::top_logits_ws_bytes(n, classes, k);
     if (need && (!ws || (uintptr_t)ws % 16)) return fail(PSW_ERR_NULL, "top_logits: needs a workspace aligned to 16 bytes");
     if (ws_bytes < need) return fail(PSW_ERR_WORKSPACE, "top_logits: workspace %zu < %zu bytes", ws_bytes, need);
@@ -582,7 +582,7 @@ int psw_distill(int n, int classes, int type, const void* logits, int64_t ld, in
     if (!(alpha >= 0.f && alpha <= 1.f)) return fail(PSW_ERR_SHAPE, "distill: alpha must be in [0, 1]");
     if (!t_idx || !t_val || (!labels && alpha != 0.f) || (!loss && !row_loss && !dlogits))
         return fail(PSW_ERR_NULL, "distill: t_idx, t_val, labels with alpha, and a result are required");
-    if (!psw::distill_fits(n, classes)) return fail(PSW_ERR_SHAPE, "distill: too many rows");
+    if (!psw::distill_fits(n, classes, type == PSW_T_BF16)) return fail(PSW_ERR_SHAPE, "distill: too many rows");
     if (dlogits) {
         const uintptr_t size = type == PSW_T_BF16 ? 2 : 4;
         if (ldd < classes) return fail(PSW_ERR_SHAPE, "distill: ldd < classes");

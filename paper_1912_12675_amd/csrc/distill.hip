@@ -613,7 +613,12 @@ size_t distill_ws_bytes(int n, int classes)
     return rows + (splits > 1 ? (size_t)n * (4 * (size_t)splits + kMost + 1) * sizeof(float) : 0);
 }
 
-bool distill_fits(int n, int classes) { return (int64_t)n * Cut(n, row_bytes(classes, 4)).splits <= INT32_MAX; }
+bool distill_fits(int n, int classes, int bf16)
+{
+    const int64_t bytes = row_bytes(classes, bf16 ? 2 : 4);  // the more, the more threads
+    const int splits = Cut(n, bytes).splits, whole = bytes <= 16 * 64 * 4 ? 64 : bytes <= 16 * 256 * 8 ? 256 : 512;
+    return (int64_t)n * (splits > 1 ? splits * 256 : whole) <= kGridThreads;
+}
 
 hipError_t distill(int n, int classes, int bf16, const void* z, int64_t ld, int k, const int32_t* idx, const float* val,
                    const float* lse, const int32_t* labels, const float* weight, float tau, float alpha, float* loss,

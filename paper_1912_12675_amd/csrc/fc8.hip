@@ -594,6 +594,24 @@ size_t mm8_ws_bytes(int M, int N, int depth)
     return parts > 1 ? (size_t)parts * M * N * sizeof(float) : 0;
 }
 
+bool mm8_fits(int M, int N, int depth, int bf16)
+{
+    auto ceil = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
+    const Plan p(M, N, (int)(q8_depth(depth) / kQ8Block), bf16);
+    int64_t threads = 0;
+    switch (p.kind) {
+    case ROWS16: threads = ceil(N, 16) * ceil(M, 16) * 512; break;
+    case ROWS32: threads = ceil(N, 16) * ceil(M, 32) * 512; break;
+    case ROWS64: threads = ceil(N, 16) * ceil(M, 64) * 512; break;
+    case TILE64: threads = ceil(ceil(M, 64) * ceil(N, 64), 8) * 8 * 256; break;
+    case WIDE: threads = ceil(ceil(M, 128) * ceil(N, 64), 8) * 8 * 256; break;
+    case TILE128: threads = ceil(ceil(M, 128) * ceil(N, 128), 8) * 8 * 256; break;
+    case TILE256: threads = ceil(ceil(M, 256) * ceil(N, 256), 8) * 8 * 256; break;
+    }
+    if (p.parts > 1) threads = std::max(threads, ceil(M * ceil(N, 4), 256) * 256);
+    return threads <= kGridThreads;
+}
+
 hipError_t mm8(int M, int N, int depth, const uint8_t* A, const uint8_t* sa, bool atiles, const uint8_t* B,
                const uint8_t* sb, bool btiles, const float* bias, int relu, void* C, int bf16, int accumulate, void* ws,
                hipStream_t st)

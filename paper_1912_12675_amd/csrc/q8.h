@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "grid.h"
+
 namespace psw {
 
 constexpr int kQ8Block = 128;
@@ -16,11 +18,13 @@ inline int q8_scales(int k) { return (int)((q8_depth(k) / kQ8Block + 3) / 4 * 4)
 inline int q8_scale_rows(int rows, bool tiles) { return tiles ? (int)(((int64_t)rows + kQ8Block - 1) / kQ8Block) : rows; }
 
 size_t q8_quant_ws_bytes(int rows, int cols);  // the column sums of the row tiles
+bool q8_quant_fits(int rows, int cols, bool rows_alone);  // its threads can be counted; without transposed rows, tiles and sums
 hipError_t q8_quant(int rows, int cols, int bf16, const void* x, int64_t ld, bool tiles, uint8_t* q, uint8_t* s,
                     uint8_t* qt, uint8_t* stp, float* colsum, void* ws, hipStream_t st);
 // C[m][n] (+)= sum_k A[m][k] B[n][k] of two 8-bit operands (atiles, btiles:
 // square blocks); bf16: C is bfloat16, else float.
 size_t mm8_ws_bytes(int M, int N, int depth);
+bool mm8_fits(int M, int N, int depth, int bf16);
 hipError_t mm8(int M, int N, int depth, const uint8_t* A, const uint8_t* sa, bool atiles, const uint8_t* B,
                const uint8_t* sb, bool btiles, const float* bias, int relu, void* C, int bf16, int accumulate, void* ws,
                hipStream_t st);

@@ -348,6 +348,12 @@ size_t q8_quant_ws_bytes(int rows, int cols)
     return parts > 1 ? (size_t)parts * cols * sizeof(double) : 0;
 }
 
+bool q8_quant_fits(int rows, int cols, bool rows_alone)
+{
+    if (rows_alone) return ((int64_t)rows * q8_scales(cols) + 31) / 32 * 256 <= kGridThreads;
+    return q8_depth(cols) / kTile * (q8_depth(rows) / kTile) <= kGridThreads / kThreads;
+}
+
 hipError_t q8_quant(int rows, int cols, int bf16, const void* x, int64_t ld, bool tiles, uint8_t* q, uint8_t* s,
                     uint8_t* qt, uint8_t* stp, float* colsum, void* ws, hipStream_t st)
 {

@@ -10,6 +10,8 @@
 
 #include <type_traits>
 
+#include "grid.h"
+
 namespace psw {
 
 typedef uint32_t Chunk __attribute__((ext_vector_type(4)));  // a value of its own, where a uint4 is four

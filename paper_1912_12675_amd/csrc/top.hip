@@ -429,14 +429,24 @@ struct Cut {
     size_t ws_bytes(int n, int k) const { return splits > 1 ? (size_t)n * splits * (k * sizeof(u64) + sizeof(float2)) : 0; }
 };
 
-// Calls f(cut) for each way in which rows of these sizes can be cut: either type, with and without a chunk more for rows
-// that begin inside one.  More bytes can mean fewer pieces (33 small ones of 128 entries turn to 17 large ones).
+// Calls f(bytes of a row) with and without a chunk more for rows that begin inside one: the launch's are one of the two.  More
+// bytes can mean fewer pieces (33 small ones of 128 entries turn to 17 large ones).
 template <typename F>
-void each_cut(int n, int classes, int k, F f)
+void each_bytes(int classes, int size, F f)
 {
-    for (int size : {2, 4})
-        for (int64_t bytes : {(int64_t)classes * size, row_bytes(classes, size)}) f(Cut(n, bytes, k));
+    f((int64_t)classes * size);
+    f(row_bytes(classes, size));
 }
+
+// Threads of a workgroup with a whole row.  Enough for groups to choose the bound from: with k of 2 k groups the list holds
+// about 1.4 k keys, with k of k groups k times the logarithm of k, which is too many from 256 on.
+int threads_of(int64_t bytes, int k)
+{
+    if (bytes <= 16 * 64 * 4 && k <= 32) return 64;
+    if (bytes <= 16 * 256 * 8 && k <= 128) return 256;
+    return bytes <= 16 * 512 * 16 ? 512 : 1024;
+}
+int merge_threads(int splits, int k) { return splits * k <= 8 * 256 ? 256 : 1024; }
 
 template <typename E>
 void launch(const TopArgs& a, int64_t bytes, const Work& w, hipStream_t st)
@@ -451,7 +461,7 @@ void launch(const TopArgs& a, int64_t bytes, const Work& w, hipStream_t st)
         else
             PSW_TOP(512, 8, true, pieces);
 #define PSW_MERGE(T, N) PSW_LAUNCH(kname("top_merge_k", T, N), w, (top_merge_k<T, N>), rows, dim3(T), 0, st, a)
-        if (a.splits * a.k <= 8 * 256)
+        if (merge_threads(a.splits, a.k) == 256)
             PSW_MERGE(256, 8);
         else if (a.splits * a.k <= 8 * 1024)
             PSW_MERGE(1024, 8);
@@ -460,17 +470,16 @@ void launch(const TopArgs& a, int64_t bytes, const Work& w, hipStream_t st)
 #undef PSW_MERGE
         return;
     }
-    // Threads enough for groups to choose the bound from: with k of 2 k groups the list holds about 1.4 k keys, with k of
-    // k groups k times the logarithm of k, which is too many from 256 on.
-    if (bytes <= 16 * 64 * 4 && a.k <= 32)
+    const int t = threads_of(bytes, a.k);
+    if (t == 64)
         PSW_TOP(64, 4, false, rows);
-    else if (bytes <= 16 * 256 * 4 && a.k <= 128)
+    else if (t == 256 && bytes <= 16 * 256 * 4)
         PSW_TOP(256, 4, false, rows);
-    else if (bytes <= 16 * 256 * 8 && a.k <= 128)
+    else if (t == 256)
         PSW_TOP(256, 8, false, rows);
-    else if (bytes <= 16 * 512 * 8)
+    else if (t == 512 && bytes <= 16 * 512 * 8)
         PSW_TOP(512, 8, false, rows);
-    else if (bytes <= 16 * 512 * 16)
+    else if (t == 512)
         PSW_TOP(512, 16, false, rows);
     else
         PSW_TOP(1024, 16, false, rows);
@@ -482,15 +491,20 @@ void launch(const TopArgs& a, int64_t bytes, const Work& w, hipStream_t st)
 size_t top_logits_ws_bytes(int n, int classes, int k)
 {
     size_t need = 0;
-    each_cut(n, classes, k, [&](const Cut& c) { need = std::max(need, c.ws_bytes(n, k)); });
+    for (int size : {2, 4})
+        each_bytes(classes, size, [&](int64_t bytes) { need = std::max(need, Cut(n, bytes, k).ws_bytes(n, k)); });
     return need;
 }
 
-bool top_logits_fits(int n, int classes, int k)
+bool top_logits_fits(int n, int classes, int k, int bf16)
 {
     int64_t most = 0;
-    each_cut(n, classes, k, [&](const Cut& c) { most = std::max(most, (int64_t)n * c.splits); });
-    return most <= INT32_MAX;
+    each_bytes(classes, bf16 ? 2 : 4, [&](int64_t bytes) {
+        const Cut c(n, bytes, k);
+        const int64_t pieces = (int64_t)c.splits * (c.per == 256 * 4 ? 256 : 512);
+        most = std::max(most, c.splits > 1 ? std::max<int64_t>(pieces, merge_threads(c.splits, k)) : threads_of(bytes, k));
+    });
+    return n * most <= kGridThreads;
 }
 
 hipError_t top_logits(int n, int classes, int bf16, const void* z, int64_t ld, int k, float tau, float* val, int32_t* idx,

@@ -2,6 +2,10 @@
 that every call here returns before a kernel would start."""
 import pytest
 
+NULL, SHAPE = -1, -2
+F32, BF16 = 0, 1
+P16 = 1 << 20  # an address that is never used
+
 
 @pytest.fixture(scope="module")
 def L():
@@ -34,3 +38,76 @@ def test_top_logits_workspace_holds_the_pieces(L):
                         assert p == 1 or need >= n * p * (8 * k + 8), (n, classes, k, size, more)
                         tried += p > 1
     assert tried > 10000
+
+
+def answer(L, rc):
+    return rc, L.psw_last_error().decode()
+
+
+# sizes whose launch has 2^32 threads, and the largest that can be counted: those are refused for what else they lack
+@pytest.mark.parametrize("type_", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("cols,tiles,both,rows,fits", [
+    (1, 0, 0, 2**27, 2**27 - 8),        # 256 threads for 32 blocks, four of a row
+    (600, 0, 0, 2**26, 2**26 - 4),      # eight blocks of a row
+    (1, 0, 1, 2**30, 2**30 - 128),      # 512 threads for 128 rows
+    (1, 1, 0, 2**30, 2**30 - 128),
+    (300, 1, 1, 2**29, 2796202 * 128)])
+def test_quantise_threads(L, cols, tiles, both, rows, fits, type_):
+    def call(rows, x):
+        q = (P16, P16, P16, P16) if both else (P16, P16, None, None)
+        return answer(L, L.psw_q8_quant(rows, cols, type_, x, cols, tiles, *q, None, None, 0, None))
+
+    rc, words = call(rows, P16)
+    assert rc == SHAPE and "too large" in words, (rc, words)
+    rc, words = call(fits, None)
+    assert rc == NULL and "required" in words, (rc, words)
+
+
+@pytest.mark.parametrize("type_", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,out,fits", [(1, 2**27, 2**27 - 16), (16, 2**28, 2**27 - 16), (40, 2**30, 2**30 - 512)])
+def test_product_threads(L, n, out, fits, type_):
+    """Few rows: 512 threads for 16 columns, above 16 rows 256 for 64."""
+    def call(out, x):
+        return answer(L, L.psw_fc8_fwd(n, 128, out, x, P16, P16, P16, None, 0, type_, P16, P16, 1 << 60, None))
+
+    rc, words = call(out, P16)
+    assert rc == SHAPE and "too large" in words, (rc, words)
+    rc, words = call(fits, None)
+    assert rc == NULL and "required" in words, (rc, words)
+
+
+ROWS = [(10, 64), (2020, 256), (10000, 512)]  # float32 classes (twice as many of bfloat16) and a row's threads
+
+
+@pytest.mark.parametrize("type_", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("classes,threads", ROWS)
+def test_rows_of_logits(L, classes, threads, type_):
+    c, n = classes * (1 + type_), 2**32 // threads
+
+    def top(n, val):
+        return answer(L, L.psw_top_logits(n, c, type_, P16, c, 5, 1.0, val, P16, None, P16, 1 << 60, None))
+
+    def loss(n, ws):
+        return answer(L, L.psw_distill(n, c, type_, P16, c, 5, P16, P16, None, None, None, 1.0, 0.0, P16, None, None, 0, ws, 1 << 60, None))
+
+    for call in (top, loss):
+        rc, words = call(n, P16)
+        assert rc == SHAPE and "too many rows" in words, (rc, words)
+        rc, words = call(n - 1, None)
+        assert rc == NULL and ("required" in words or "workspace" in words), (rc, words)
+
+
+@pytest.mark.parametrize("type_", [F32, BF16], ids=["f32", "bf16"])
+def test_rows_in_pieces(L, type_):
+    """2^20 classes: 4 or 2 MB and up to 16 bytes more, in 65 or 33 pieces of 512 threads (top logits), in 129 or 65 of 256
+    (the loss)."""
+    c, pieces = 1 << 20, 33 if type_ else 65
+    for n, want in ((2**32 // (pieces * 512) + 1, SHAPE), (2**32 // (pieces * 512) - 1, NULL)):
+        rc, words = answer(L, L.psw_top_logits(n, c, type_, P16, c, 256, 1.0, P16 if want == SHAPE else None, P16, None, P16,
+                                               1 << 60, None))
+        assert rc == want, (rc, words)
+    pieces = 65 if type_ else 129
+    for n, want in ((2**32 // (pieces * 256) + 1, SHAPE), (2**32 // (pieces * 256) - 1, NULL)):
+        rc, words = answer(L, L.psw_distill(n, c, type_, P16, c, 5, P16, P16, None, None, None, 1.0, 0.0, P16, None, None, 0,
+                                            P16 if want == SHAPE else None, 1 << 60, None))
+        assert rc == want, (rc, words)
