@@ -321,10 +321,11 @@ size_t psw_distill_ws_bytes(int n, int classes);
  *   loss = sum_i weight[i] row_loss[i]         (one device float)
  *   dlogits[i][j] = weight[i] d row_loss[i] / d z_j   (rows `ldd` apart)
  * An entry whose class is outside [0, classes) or whose logit is -inf is
- * absent; a class given more than once counts once, with the sum of its p; a
- * row without entries has no soft term, one whose label is outside [0, classes)
- * no hard term.  Where every class outside a row's entries has z = -inf, or there
- * is none, r is not counted.
+ * absent, and every entry where alpha is 1 (row_loss is then hard alone, whatever
+ * the entries hold), as labels are where alpha is 0; a class given more than
+ * once counts once, with the sum of its p; a row without entries has no soft
+ * term, one whose label is outside [0, classes) no hard term.  Where every class
+ * outside a row's entries has z = -inf, or there is none, r is not counted.
  * weight NULL: 1 / n each.  Where weight[i] is 0 the row's logits are not looked
  * at: row_loss[i] and its gradient are 0.  A row whose logits are all -inf, or
  * hold NaN or +inf, has no softmax: NaN.

@@ -129,7 +129,7 @@ __global__ __launch_bounds__(T, waves_of(T, NV)) void distill_k(DistillArgs a)
     z.template load<T>(v, c0, lo, FORM == GRADIENT && !a.d ? lo : hi);
     float xs = es >= 0 ? (float)z.p[es] : -INFINITY;
 
-    // the teacher's entries, up to KI a thread
+    // the teacher's entries, up to KI a thread; none where the loss is the label's (0 times an infinite loss is NaN)
     const int label = a.labels ? a.labels[row] : -1;
     const bool has = a.alpha != 0.f && label >= 0 && label < a.classes;
     int idx[KI];
@@ -144,7 +144,7 @@ __global__ __launch_bounds__(T, waves_of(T, NV)) void distill_k(DistillArgs a)
         if (k < a.k) {
             const int e = a.idx[(int64_t)row * a.k + k];
             val[i] = a.val[(int64_t)row * a.k + k];
-            if (e >= 0 && e < a.classes && !(val[i] == -INFINITY)) {
+            if (e >= 0 && e < a.classes && !(val[i] == -INFINITY) && a.alpha != 1.f) {
                 idx[i] = e;
                 zk[i] = FORM == GRADIENT ? kept[k] : (float)z.p[e];
                 if (FORM == PIECE && piece == 0) kept[k] = zk[i];

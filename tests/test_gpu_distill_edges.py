@@ -1,10 +1,10 @@
 """Top logits and the distillation loss where their rules change: workspaces of exactly the bytes that are asked for, masked
-pieces of rows far from zero."""
+pieces of rows far from zero, a loss of labels alone."""
 import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_distill import check_top, matrix, top_ref
+from tests.test_gpu_distill import check_distill, check_top, distill_ref, matrix, run, top_ref
 
 pytestmark = pytest.mark.gpu
 
@@ -66,3 +66,29 @@ def test_masked_pieces_far_from_zero(P, n, c, k, pad, tau, at, spread, masked, t
         P.psw_distill(z, idx, val, row_loss=row, t_lse=lse, temperature=tau)
         torch.cuda.synchronize()
         assert bool(torch.isfinite(row).all())
+
+
+@pytest.mark.parametrize("tail", [False, True], ids=["entries", "rest"])
+@pytest.mark.parametrize("type_", ["f32", "bf16"])
+@pytest.mark.parametrize("n,c,k", [(6, 50, 7), (4, 900, 64), (3, 40000, 60), (3, 140000, 60)])
+def test_labels_alone(P, n, c, k, type_, tail):
+    """alpha 1: the loss is the label's, whatever the teacher says of classes that the student masks."""
+    print(f"labels alone {n}x{c} k {k} {type_} rest={tail}", flush=True)
+    rng = np.random.default_rng(c)
+    z = rng.standard_normal((n, c)) * 2
+    z[0, : c // 2] = -np.inf
+    z[1, 5] = -np.inf
+    x, _ = matrix(z, type_)
+    z = x.double().cpu().numpy()
+    idx = np.tile(np.arange(k, dtype=np.int32), (n, 1))
+    val = rng.standard_normal((n, k)).astype(np.float32)
+    lse = np.full(n, 6.0, np.float32)
+    val[2, 1], lse[2] = np.nan, np.inf
+    label = rng.integers(c // 2, c, n).astype(np.int32)
+    weight = rng.uniform(0.5, 2, n).astype(np.float32)
+    dz, _ = matrix(np.full((n, c), 7.0), type_)
+    got = run(P, x, idx, val, lse if tail else None, label, weight, 3.0, 1.0, dz)
+    val[2], lse[2] = 0.0, 6.0
+    idx[:] = -1  # the formulas without their first terms
+    ref = distill_ref(z, idx, val, None, label, weight.astype(np.float64), 3.0, 1.0)
+    check_distill(got, dz, ref, weight.astype(np.float64), type_, "alpha 1")
