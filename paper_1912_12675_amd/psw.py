@@ -373,6 +373,13 @@ def _here(t, what):
         raise ValueError(f"{what} is on {t.device}, not on the current device")
 
 
+def _size(*sizes):
+    """Sizes as the library counts them: ctypes would keep their low 32 bits."""
+    for v in sizes:
+        if v >= 2**31:
+            raise ValueError(f"a size of {v}: sizes are below 2^31")
+
+
 def _mat(t, what, shape=None):
     """(pointer, type, elements from row to row) of a float32 / bfloat16 device matrix whose rows are contiguous."""
     _here(t, what)
@@ -380,6 +387,7 @@ def _mat(t, what, shape=None):
         raise TypeError(f"{what} is float32 or bfloat16, got {t.dtype}")
     if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
         raise ValueError(f"{what} has shape {tuple(t.shape)}, not {'two dimensions' if shape is None else tuple(shape)}")
+    _size(*t.shape)
     if t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{what} takes contiguous rows")
     ld = t.stride(0) if t.shape[0] > 1 else t.shape[1]
@@ -406,6 +414,7 @@ def _q8_shapes(rows, k, tiles):
 
 
 def _q8(q, s, what, rows, k, tiles):
+    _size(rows, k)
     if q is None and s is None:
         return None, None
     vq, vs = _q8_shapes(rows, k, tiles)
@@ -509,6 +518,7 @@ def psw_top_logits(logits, val, idx, temperature=1.0, lse=None, ws=None, stream=
         return _check(rc)
     n, classes = logits.shape
     k = val.shape[1]
+    _size(k)
     pz, type_, ld = _mat(logits, "logits")
     wp, nb, ws = _space(ws, lambda: psw_top_logits_ws_bytes(n, classes, k), stream)
     _check(lib().psw_top_logits(n, classes, type_, pz, ld, k, temperature, _vec(val, "val", torch.float32, n, k),
@@ -529,6 +539,7 @@ def psw_distill(logits, t_idx, t_val, loss=None, dlogits=None, labels=None, weig
         return _check(rc)
     n, classes = logits.shape
     k = t_idx.shape[1]
+    _size(k)
     pz, type_, ld = _mat(logits, "logits")
     pd, ldd = None, 0
     if dlogits is not None:

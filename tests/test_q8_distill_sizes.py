@@ -1,6 +1,7 @@
 """Sizes of the 8-bit products, the top logits and the distillation loss at the edges of their rules: host checks alone, so
 that every call here returns before a kernel would start."""
 import pytest
+import torch
 
 NULL, SHAPE = -1, -2
 F32, BF16 = 0, 1
@@ -111,3 +112,33 @@ def test_rows_in_pieces(L, type_):
         rc, words = answer(L, L.psw_distill(n, c, type_, P16, c, 5, P16, P16, None, None, None, 1.0, 0.0, P16, None, None, 0,
                                             P16 if want == SHAPE else None, 1 << 60, None))
         assert rc == want, (rc, words)
+
+
+def test_sizes_past_31_bits(monkeypatch):
+    """ctypes keeps the low bits of an integer: a size of 2^32 + 5 would be one of 5."""
+    from paper_1912_12675_amd import psw
+
+    monkeypatch.setattr(psw, "_here", lambda t, what: None)  # tensors without memory in the place of a device's
+    monkeypatch.setattr(psw, "_fast", psw._CtypesOnly())
+    many = 2**32 + 5
+
+    def new(*shape, dtype=torch.float32):
+        return torch.empty(*shape, dtype=dtype, device="meta")
+
+    def op(rows, k, tiles=False):
+        return psw.q8_operand(rows, k, tiles, device="meta")
+
+    i32 = torch.int32
+    for call in (lambda: psw.psw_q8_quant(new(many, 1), None, None, *op(1, many)),
+                 lambda: psw.psw_q8_quant(new(1, many), colsum=new(many), ws=new(8)),
+                 lambda: psw.psw_fc8_fwd(op(1, many), op(3, many, True), many, new(1, 3), ws=new(8)),
+                 lambda: psw.psw_fc8_fwd(op(many, 1), op(3, 1, True), 1, new(many, 3), ws=new(8)),
+                 lambda: psw.psw_fc8_bwd_data(op(1, many), op(3, many, True), many, new(1, 3), ws=new(8)),
+                 lambda: psw.psw_fc8_bwd_weight(op(3, many), op(2, many), many, new(3, 2), ws=new(8)),
+                 lambda: psw.psw_fc8_bwd_weight(op(many, 1), op(2, 1), 1, new(many, 2), ws=new(8)),
+                 lambda: psw.psw_top_logits(new(many, 3), new(many, 2), new(many, 2, dtype=i32), ws=new(8)),
+                 lambda: psw.psw_top_logits(new(2, 3), new(2, many), new(2, many, dtype=i32), ws=new(8)),
+                 lambda: psw.psw_distill(new(many, 3), new(many, 2, dtype=i32), new(many, 2), new(1), ws=new(8)),
+                 lambda: psw.psw_distill(new(2, 3), new(2, many, dtype=i32), new(2, many), new(1), ws=new(8))):
+        with pytest.raises(ValueError, match="below 2.31"):
+            call()
