@@ -1,4 +1,5 @@
-"""8-bit operands and products at the ends of their range, and what the 8-bit instruction drops."""
+"""8-bit operands and products at the ends of their range, what the 8-bit instruction drops, and column
+sums of one rounding."""
 import numpy as np
 import pytest
 import torch
@@ -136,3 +137,29 @@ def test_bfloat16_products_in_the_norm(P, n, fin, out):
     d = 7e-5 * square
     off = (y.double() - want.to(torch.bfloat16).double()).square().sum()
     assert float(off) <= 2 * float((d * 2.0**-7 * want.abs() + d.square()).sum())
+
+
+@pytest.mark.parametrize("type_", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(1, 5), (128, 130), (129, 9), (1000, 257), (5000, 3)])
+def test_column_sums_round_once(P, rows, cols, type_):
+    """Column sums are formed in 64 bits from the first row on: fewer than rows + 40 additions, each off by at most
+    half a step, 2^-53 of what is there, and one rounding to float32."""
+    print(f"column sums {rows}x{cols} {type_}", flush=True)
+    rng = np.random.default_rng(rows + cols)
+    x = rng.standard_normal((rows, cols)) * np.exp(3 * rng.standard_normal((rows, cols)))
+    if rows > 1:  # large numbers that cancel
+        x[0, 0] = 2.0**30
+        x[rows - 1, 0] = -(2.0**30)
+        x[1:rows // 2 + 1, cols - 1] = -x[rows - rows // 2:, cols - 1][::-1]
+    xt = torch.from_numpy(x.astype(np.float32)).cuda().to(TYPES[type_])
+    x = xt.double().cpu().numpy().astype(np.longdouble)
+    total = torch.zeros(cols, device="cuda")
+    P.psw_q8_quant(xt, colsum=total)
+    q = P.q8_operand(cols, rows)
+    again = torch.zeros(cols, device="cuda")
+    P.psw_q8_quant(xt, qt=q[0], st=q[1], colsum=again)
+    torch.cuda.synchronize()
+    assert torch.equal(total, again)
+    want, size = x.sum(0), np.abs(x).sum(0)
+    bound = 2.0**-24 * np.abs(want) + (1 + 2.0**-24) * (rows + 40) * 2.0**-53 * size + 2.0**-149
+    assert (np.abs(total.double().cpu().numpy() - want) <= bound).all()
