@@ -289,7 +289,7 @@ int psw_fc8_bwd_weight(int n, int in, int out, const uint8_t *dytq, const uint8_
 #define PSW_MAX_CLASSES (1 << 20) /* of the two entry points below */
 #define PSW_MAX_TOP 256
 
-/* Workspace bytes of psw_top_logits (0 for many rows of moderate length). */
+/* Workspace bytes of psw_top_logits (0 for up to 65532 classes: rows of 256 KB). */
 size_t psw_top_logits_ws_bytes(int n, int classes, int k);
 
 /* The k largest of each row of logits [n][classes] of `type`, rows `ld` elements

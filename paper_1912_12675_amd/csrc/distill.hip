@@ -3,10 +3,10 @@
 //
 // A workgroup holds its row of logits in registers, so that memory sees each
 // logit once and each gradient once: the largest logit, the sums of
-// exponentials, then the gradient, all from there.  Rows that are too long are
-// cut into pieces of 8 or 32 KB, whose maxima and sums
-// (`distill_k` in its second form) the gradient's workgroups (third form) put
-// together in order.
+// exponentials, then the gradient, all from there.  Rows past 128 KB are cut into
+// pieces of 8 or 32 KB, whose maxima and sums (`distill_k` in its second form) the
+// gradient's workgroups (third form), which read the logits again, put together
+// in order: 1024 rows of 100000 bfloat16 63 + 84 us.
 //
 // What the teacher says about the rest of the classes is a probability, r, for
 // all of them together; the student's probability of the rest, R, is summed

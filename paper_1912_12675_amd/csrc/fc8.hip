@@ -155,13 +155,15 @@ __device__ __forceinline__ void weave()
 // The 16-byte unit u of row r lies in place u ^ (r / 2 & 7): a wave's loads fill
 // eight rows in lane order (each lane fetches the unit that belongs in its
 // place), and the 16 lanes that LDS serves in a cycle meet no bank twice.
-// Bound by the matrix cores and the power they draw where tiles are many: 8192 x
-// 4096 -> 16384 bfloat16 450 to 530 us by card and clock (2.1 to 2.4 PFLOP/s; a
-// tile's first loads and last stores, 12 us of each of the eight rounds, are not hidden),
-// 4096 x 16384 -> 8192 float32 724 us (1.52 PFLOP/s).  With few tiles by the
+// Bound by the matrix cores and the power they draw where tiles are many, at 1.7
+// GHz: 4096 x 16384 -> 8192 float32 724 to 783 us by card and clock (1.4 to 1.52
+// PFLOP/s; the matrix cores are busy in 82% of a CU's cycles), 8192 x 4096 -> 16384
+// bfloat16 450 to 550 us (2.0 to 2.4 PFLOP/s; 60%: a tile's first loads and last
+// stores, 12 us of each of the eight rounds, are not hidden).  With few tiles by the
 // operand that is read once: 128 x 16384 -> 4096 25 us for 69 MB, of which 14
 // are the bytes, the rest the conversions of 96 operands for 16 matrix
-// instructions and the rows' 128 bytes at a time from HBM.
+// instructions and the rows' 128 bytes at a time from HBM; the same number of
+// tiles and blocks with rows 4 KB apart (dx of that layer) 37 us.
 // The matrix instruction's rows are C's columns, so that a lane ends with four
 // neighbours of a row of C; a wave's rows turn in LDS and are stored whole.
 template <int BM, int BN, int WM, int WN, int D, bool F8>

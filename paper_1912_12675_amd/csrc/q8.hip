@@ -87,11 +87,12 @@ __device__ __forceinline__ float4 load4(const T* p)
 // Both orders, column sums, or square blocks: a 128 x 128 tile.  A thread holds
 // two pieces of 4 rows x 4 columns (32 threads side by side read 128 columns of
 // a row): 512 threads a tile leave two to four tiles a CU, of which one loads
-// while others turn (bfloat16 three rather than two: 8192 x 4096 35.5 us, so 34, and 36 with the largest scale's question;
-// float32, whose tiles are twice the bytes, 41 us, with three 47).  Bound by
-// memory: 16384 x 4096 float32, square blocks, 80 us (5.0 TB/s), 8192 x 4096 by
-// rows and columns with sums 41 us (4.9 TB/s); 2047 x 4104 so 17 us (2.9 TB/s;
-// its 528 tiles are one round of the chip and 16 more).
+// while others turn (bfloat16 three rather than two: 8192 x 4096 35.5 us, so 34,
+// and 36 with the largest scale's question; float32, whose tiles are twice the
+// bytes, 41 us, with three 47).  Bound by memory: 16384 x 4096 float32, square
+// blocks, 80 us (5.0 TB/s), 8192 x 4096 by rows and columns with sums 41 us (4.9
+// TB/s); 2047 x 4104 so 17 us (2.9 TB/s; its 528 tiles are one round of the chip
+// and 16 more).
 template <typename T, bool TILES>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 6 : 4) void q8_quant_k(QuantArgs a)
 {

@@ -4,7 +4,7 @@
 // A number and its class make one 64-bit key, larger for the larger number and,
 // among equal ones, for the lower class, so no two keys are equal and the result
 // is one set in one order.  A workgroup holds its row in registers (rows.h).
-// The k-th largest of the maxima of 128 or more groups of threads is at most the
+// The k-th largest of the maxima of 64 or more groups of threads is at most the
 // row's k-th largest.  The few chunks whose largest element is from there up go
 // to a list in LDS, their elements from there up to a list of keys, and a key's
 // place is the number of larger ones there.
