@@ -330,8 +330,8 @@ size_t psw_distill_ws_bytes(int n, int classes);
  * at: row_loss[i] and its gradient are 0.  A row whose logits are all -inf, or
  * hold NaN or +inf, has no softmax: NaN.
  * labels may be NULL if alpha is 0; loss, row_loss and dlogits may be NULL, not
- * all three.  dlogits may be logits (with ldd == ld), but not overlap it
- * otherwise.  0 <= alpha <= 1, 2^-16 <= temperature <= 2^16, 1 <= k <= PSW_MAX_TOP.
+ * all three.  dlogits may be logits (with ldd == ld), or columns of the same
+ * matrix beside them, but not overlap them otherwise.  0 <= alpha <= 1, 2^-16 <= temperature <= 2^16, 1 <= k <= PSW_MAX_TOP.
  * Sums are formed in a fixed order: results are bit-reproducible. */
 int psw_distill(int n, int classes, int type, const void *logits, int64_t ld, int k,
                 const int32_t *t_idx, const float *t_val, const float *t_lse, const int32_t *labels,

@@ -587,9 +587,12 @@ int psw_distill(int n, int classes, int type, const void* logits, int64_t ld, in
         const uintptr_t size = type == PSW_T_BF16 ? 2 : 4;
         if (ldd < classes) return fail(PSW_ERR_SHAPE, "distill: ldd < classes");
         if ((uintptr_t)dlogits % size) return fail(PSW_ERR_SHAPE, "distill: dlogits must be aligned to its elements");
-        const uintptr_t z0 = (uintptr_t)logits, d0 = (uintptr_t)dlogits;
-        const uintptr_t z1 = z0 + ((uintptr_t)(n - 1) * ld + classes) * size, d1 = d0 + ((uintptr_t)(n - 1) * ldd + classes) * size;
-        if (z0 < d1 && d0 < z1 && !(z0 == d0 && ld == ldd))
+        const uintptr_t z0 = (uintptr_t)logits, d0 = (uintptr_t)dlogits, row = (uintptr_t)classes * size, pitch = (uintptr_t)ld * size;
+        const uintptr_t z1 = z0 + (uintptr_t)(n - 1) * pitch + row, d1 = d0 + (uintptr_t)(n - 1) * ldd * size + row;
+        // side by side: columns of one matrix
+        const uintptr_t in = d0 >= z0 ? (d0 - z0) % pitch : (pitch - (z0 - d0) % pitch) % pitch;
+        const bool beside = ld == ldd && in >= row && in + row <= pitch;
+        if (z0 < d1 && d0 < z1 && !(z0 == d0 && ld == ldd) && !beside)
             return fail(PSW_ERR_SHAPE, "distill: dlogits overlaps logits");
     }
     const size_t need = psw::distill_ws_bytes(n, classes);

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_distill import check_distill, check_top, distill_ref, matrix, run, top_ref
+from tests.test_gpu_distill import TYPES, check_distill, check_top, distill_ref, matrix, run, teacher, top_ref
 
 pytestmark = pytest.mark.gpu
 
@@ -92,3 +92,25 @@ def test_labels_alone(P, n, c, k, type_, tail):
     idx[:] = -1  # the formulas without their first terms
     ref = distill_ref(z, idx, val, None, label, weight.astype(np.float64), 3.0, 1.0)
     check_distill(got, dz, ref, weight.astype(np.float64), type_, "alpha 1")
+
+
+@pytest.mark.parametrize("type_", ["f32", "bf16"])
+@pytest.mark.parametrize("n,c,gap", [(5, 100, 0), (4, 1003, 5), (3, 40000, 1), (2, 70001, 3)])
+def test_gradients_beside_logits(P, n, c, gap, type_):
+    """Logits and gradients as columns of one matrix, either first; nothing else is written."""
+    print(f"beside {n}x{c} gap {gap} {type_}", flush=True)
+    rng = np.random.default_rng(c)
+    tau, alpha = 2.0, 0.3
+    label, weight = rng.integers(0, c, n).astype(np.int32), rng.uniform(0.5, 2, n).astype(np.float32)
+    for first in (True, False):
+        both = torch.full((n, 2 * c + 2 * gap), 7.0, dtype=TYPES[type_], device="cuda")
+        left, right = both[:, :c], both[:, c + gap:2 * c + gap]
+        x, d = (left, right) if first else (right, left)
+        x.copy_(torch.from_numpy(rng.standard_normal((n, c)) * 3))
+        z = x.double().cpu().numpy()
+        idx, val, lse = teacher(rng, z, 7, tau, "odd")
+        got = run(P, x, idx, val, lse, label, weight, tau, alpha, d)
+        ref = distill_ref(z, idx, val, lse.astype(np.float64), label, weight.astype(np.float64), tau, alpha)
+        check_distill(got, d, ref, weight.astype(np.float64), type_, "beside")
+        assert np.array_equal(x.double().cpu().numpy(), z)
+        assert bool((both[:, c:c + gap] == 7).all()) and bool((both[:, 2 * c + gap:] == 7).all())

@@ -142,3 +142,20 @@ def test_sizes_past_31_bits(monkeypatch):
                  lambda: psw.psw_distill(new(2, 3), new(2, many, dtype=i32), new(2, many), new(1), ws=new(8))):
         with pytest.raises(ValueError, match="below 2.31"):
             call()
+
+
+@pytest.mark.parametrize("type_", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,ld,ldd,at,fine", [  # dlogits `at` elements behind the logits, rows of 100
+    (4, 200, 200, 100, True), (4, 200, 200, -100, True), (4, 250, 250, 120, True), (4, 250, 250, 350, True),
+    (4, 250, 250, 150, True), (4, 250, 250, -350, True), (4, 200, 200, 0, True), (4, 100, 100, 400, True),
+    (1, 100, 100, 100, True), (4, 100, 100, -400, True),
+    (4, 200, 200, 99, False), (4, 200, 200, 101, False), (4, 250, 250, 151, False), (4, 250, 250, -151, False),
+    (4, 200, 201, 100, False), (4, 201, 200, -100, False), (4, 100, 100, 100, False), (4, 250, 250, 250, False),
+    (1, 100, 100, 99, False), (4, 100, 100, 399, False)])
+def test_gradients_beside_logits(L, n, ld, ldd, at, fine, type_):
+    """Columns of one matrix do not overlap, however their rows lie."""
+    z = P16
+    dz = z + at * (2 if type_ == BF16 else 4)
+    rc, words = answer(L, L.psw_distill(n, 100, type_, z, ld, 5, P16, P16, None, None, None, 1.0, 0.0, P16, None, dz, ldd, None,
+                                        0, None))
+    assert (rc == NULL and "workspace" in words) if fine else (rc == SHAPE and "overlaps" in words), (rc, words)
