@@ -328,7 +328,8 @@ size_t psw_distill_ws_bytes(int n, int classes);
  * outside a row's entries has z = -inf, or there is none, r is not counted.
  * weight NULL: 1 / n each.  Where weight[i] is 0 the row's logits are not looked
  * at: row_loss[i] and its gradient are 0.  A row whose logits are all -inf, or
- * hold NaN or +inf, has no softmax: NaN.
+ * hold NaN or +inf, has no softmax: its gradient and what terms its loss has are
+ * NaN.
  * labels may be NULL if alpha is 0; loss, row_loss and dlogits may be NULL, not
  * all three.  dlogits may be logits (with ldd == ld), or columns of the same
  * matrix beside them, but not overlap them otherwise.  0 <= alpha <= 1, 2^-16 <= temperature <= 2^16, 1 <= k <= PSW_MAX_TOP.
